@@ -477,13 +477,15 @@ def _matrix(t, dtype, name):
     return ld
 
 
-def _codes_check(w, w_scale, K, name):
-    """(rows, elements between rows) of int8 codes that hold K columns, padded to 16."""
+def _codes_check(w, w_scale, K, name, longer=False):
+    """(rows, elements between rows) of int8 codes that hold K columns, padded to 16, and no more
+    unless rows may be longer."""
     ld = _matrix(w, torch.int8, name)
     _arg(w_scale, torch.float32, name + "_scale")
     rows, cols = w.shape
-    if cols < (K + 15) // 16 * 16:
-        raise FastRLError(f"{name}: {K} columns need {(K + 15) // 16 * 16} codes a row")
+    need = (K + 15) // 16 * 16
+    if cols < need or (cols > need and not longer):
+        raise FastRLError(f"{name}: {K} columns need {need} codes a row, got {cols}")
     if w_scale.numel() != rows:
         raise FastRLError(f"{name}_scale: expected one scale for each of {rows} rows")
     return rows, ld
@@ -517,9 +519,10 @@ def matmul_i8(x, x_scale, w, w_scale, *, K=None, out_dtype=None, out=None):
     """Product of int8 codes ``x`` [T, Kp] and ``w`` [N, Kp] (see ``quantize_rows``) with a scale
     per token and output channel: [T, N] in ``out_dtype`` (bfloat16 if not given) or into
     ``out``, whose rows may be strided.  ``K``: columns that count (all of x's if not given)."""
-    K = x.shape[1] if K is None else K
-    T, ldx = _codes_check(x, x_scale, K, "x")
-    N, ldw = _codes_check(w, w_scale, K, "w")
+    stated = K is not None
+    K = K if stated else x.shape[1]
+    T, ldx = _codes_check(x, x_scale, K, "x", longer=stated)
+    N, ldw = _codes_check(w, w_scale, K, "w", longer=stated)
     out, ldo = _out(out, T, N, out_dtype, x)
     _check(_lib.fastrl_matmul_i8(x.data_ptr(), ldx, x_scale.data_ptr(), w.data_ptr(), ldw,
                                  w_scale.data_ptr(), T, N, K, out.data_ptr(), _dtype_code(out),
