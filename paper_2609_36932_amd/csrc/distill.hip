@@ -44,8 +44,9 @@ struct DistillParams {
   void* E;                // NULL without a backward
   int64_t ldE;
   int32_t bf16;
-  const float* shift;     // of the slab (NULL without a backward)
-  const float* sum;       // [Tc] sum exp(z / tau - s) (with a backward)
+  const float* shift;     // of the slab (without a backward: the token's maximum of z / tau)
+  const float* sum;       // [Tc] sum exp(z / tau - s)
+  const float* pmax;      // [nmb][ldp] maxima of the vocabulary blocks
   const float* psum;      // partials of rows evaluated again
   int64_t ldp;
   int32_t nmb;
@@ -118,7 +119,7 @@ __device__ __forceinline__ double wave_sum_d(double v) {
 __device__ __forceinline__ void distill_token(const DistillParams& p, int tl) {
   const int lane = threadIdx.x & 63;
   const int64_t t = p.t0 + tl;
-  const float s_t = p.shift ? p.shift[tl] : 0.0f;
+  const float s_t = p.shift[tl];
   const double tau_inv = p.zscale;
   int y[2];
   double x[2], q[2], logq[2], logp[2];
@@ -148,25 +149,24 @@ __device__ __forceinline__ void distill_token(const DistillParams& p, int tl) {
   // The student's log-sum-exp from the sum of float32 exponentials (of a row evaluated again: from its
   // new partials).  Their errors grow with z: at z / tau = 60 the exponent alone rounds by 4e-6, and a
   // student close to its teacher has most of the sum in the teacher's entries.  So those are put
-  // right: their float32 exponentials, formed here as the GEMM's epilogue does, are replaced.
-  double l = p.lse[t];
-  if (p.shift) {
-    double S = p.sum[tl], fix = 0.0;
-    if (s_t != 0.0f && p.redo_any[0] != 0) {
-      S = 0.0;
-      for (int m = lane; m < p.nmb; m += 64) S += double(p.psum[int64_t(m) * p.ldp + tl]);
-      S = wave_sum_d(S);
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-      if (own[u]) {
-        const float e = p.bf16 ? __builtin_amdgcn_exp2f(fmaf(z[u], 1.4426950408889634f, -(s_t * 1.4426950408889634f)))
-                               : __expf(z[u] - s_t);
-        fix += exp(double(z[u]) - double(s_t)) - double(e);
-      }
-    l = double(s_t) + log(S + wave_sum_d(fix));
-    if (lane == 0) p.lse[t] = float(l);
+  // right: their float32 exponentials, formed here as the GEMM's epilogue does, are replaced.  Without a
+  // backward that one forms them relative to the block's maximum, which the merge brings to the token's.
+  double S = p.sum[tl], fix = 0.0;
+  if (p.E && s_t != 0.0f && p.redo_any[0] != 0) {
+    S = 0.0;
+    for (int m = lane; m < p.nmb; m += 64) S += double(p.psum[int64_t(m) * p.ldp + tl]);
+    S = wave_sum_d(S);
   }
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    if (own[u]) {
+      const float ref = p.E ? s_t : p.pmax[int64_t(y[u] >> 8) * p.ldp + tl];
+      const float e = p.bf16 ? __builtin_amdgcn_exp2f(fmaf(z[u], 1.4426950408889634f, -(ref * 1.4426950408889634f)))
+                             : __expf(z[u] - ref);
+      fix += exp(double(z[u]) - double(s_t)) - double(e) * (p.E ? 1.0 : exp(double(ref) - double(s_t)));
+    }
+  const double l = double(s_t) + log(S + wave_sum_d(fix));
+  if (lane == 0) p.lse[t] = float(l);
   double L = 0.0;
   if (p.tlse) {
     L = p.tlse[t];
@@ -363,7 +363,7 @@ static int run_distill(const fastrl_distill_args& a, hipStream_t stream) {
   p.zscale = 1.0f / a.temperature;
   p.sid = w.sid; p.sa = w.sa; p.off = w.off; p.zk = w.zk; p.lse = w.lse; p.token_loss = w.token_loss; p.term = w.term; p.cslab = w.cslab;
   p.E = store ? w.E1 : nullptr; p.ldE = rup(a.V, kBM); p.bf16 = a.dtype == FASTRL_BF16;
-  p.shift = store ? w.shift : nullptr; p.sum = w.sum; p.psum = w.psum; p.ldp = lc.tcp;
+  p.shift = w.shift; p.sum = w.sum; p.pmax = w.pmax; p.psum = w.psum; p.ldp = lc.tcp;
   p.nmb = int32_t(rup(a.V, kBM) / kBM); p.status = a.status;
   for (int64_t i = 0; i < slabs.n && a.T > 0; ++i) {
     const int64_t t0 = a.T * i / slabs.n;

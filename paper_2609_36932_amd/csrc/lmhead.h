@@ -25,7 +25,8 @@ struct LmWs {
   void *WT = nullptr, *E1 = nullptr, *Bd = nullptr;
   float *pmax = nullptr, *psum = nullptr, *psz = nullptr, *zlab = nullptr, *shift = nullptr, *cslab = nullptr;
   int32_t *yslab = nullptr, *redo_blk = nullptr, *redo_count = nullptr;
-  float* sum = nullptr;  // NULL, or sum exp(z - s_t) of each token (with a gradient asked for)
+  // NULL, or sum exp(z - s_t) of each token; without a gradient asked for, s_t (shift) is the token's maximum then
+  float* sum = nullptr;
   // NULL, or given ids, a row of pick_n per slab token: ascending, where those of each 256 vocabulary rows begin
   // (and, last, end) and their logits
   const int32_t* pick_ids = nullptr;

@@ -1046,7 +1046,10 @@ __global__ __launch_bounds__(32 * SLICES) void merge_kernel(
   const float l = rel ? s_t + __logf(S) : M + __logf(S);
   const int y = yslab[t];
   if (lse_out) lse_out[t] = l;
-  if (sum_out) sum_out[t] = S;
+  if (sum_out) {
+    sum_out[t] = S;
+    if (!rel) shift[t] = M;  // what S is relative to
+  }
   if (logp_out) logp_out[t] = y >= 0 ? zlab[t] - l : __int_as_float(0x7fc00000);
   // entropy -sum_v p_v log p_v = lse - sum_v p_v z_v, sum_v p_v z_v = Z / S
   if (ent_out) ent_out[t] = l - Z / S;
@@ -1871,8 +1874,8 @@ static int lm_forward_t(const LmCall& a, const LmWs& w, int64_t t0, int32_t Tc, 
   FR_TRY((launch_gemm<T, MODE_FWD>(p, FASTRL_K_LOGITS_FWD, 2.0 * double(a.V) * Tc * a.d, stream)));
   FR_TRY(launch_merge(w.pmax, w.psum, w.psz, a.tcp, nmb, w.zlab, w.yslab, Tc, store, lse + t0,
                       logp ? logp + t0 : nullptr, ent ? ent + t0 : nullptr,
-                      store ? w.shift : nullptr, w.redo_blk, w.redo_count, w.redo_blk + nnb,
-                      store ? w.sum : nullptr, stream));
+                      store || w.sum ? w.shift : nullptr, w.redo_blk, w.redo_count, w.redo_blk + nnb,
+                      w.sum, stream));
   // token blocks holding a row that needs a shift: evaluate again (returns at once on the device
   // when no row was marked); the loss kernels merge those rows
   if (store) FR_TRY(launch_redo<T>(p, stream));
