@@ -46,13 +46,13 @@ namespace fastrl {
 // to the block max.  A column's 256 rows are spread over the 4 lane groups of two wavefronts:
 // lane-row swaps, then one LDS exchange between the wavefronts.
 //
-// EPI_PICK (EPI_EITHER: if p.pick_z): logits times p.zscale, and those of given ids (p.pick_*) written out:
+// EPI_SCALE: logits times p.zscale.  EPI_PICK (EPI_EITHER: if p.pick_z): and those of given ids (p.pick_*) written out:
 // where a column's begin is loaded first, its first four ids with the others' after that, and 16 columns
 // at a time go through a wavefront's own LDS, where each id's logit is one read.  Against reading the ids'
 // rows of W again, with 64 ids a token: distillation of 16384 tokens at 7B 41.57 -> 40.27 ms, of 1975 5.44 ->
 // 5.36; against choosing among a lane's 32 values once per id: 2000 tokens, 128 ids, d = 896, V = 32000 431 -> 386
 // us, d = 1536, V = 8000 235 -> 190, the larger vocabularies level.
-enum FwdEpilogue { EPI_PLAIN = 0, EPI_PICK = 1, EPI_EITHER = 2 };
+enum FwdEpilogue { EPI_PLAIN = 0, EPI_PICK = 1, EPI_EITHER = 2, EPI_SCALE = 3 };
 template <int NJ, int EPI>
 __device__ __forceinline__ void fwd_epilogue_bf16(const GemmParams& p, int m0, int n0, int mb,
                                                   f32x4_t (&acc)[8][NJ], uint16_t* smem) {
@@ -906,7 +906,7 @@ void lm_redo_kernel(const GemmParams p) {
     int mb, nb;
     tile_coords<MODE_FWD>(mb, nb, p.nmb, p.nnb, b, p.group);
     if (p.redo_blk[nb] == 0) continue;  // the same for the whole block
-    fwd_tile<4, EPI_EITHER>(p, mb, nb * kBN, smem);
+    fwd_tile<4, EPI_SCALE>(p, mb, nb * kBN, smem);
     __syncthreads();  // the epilogue's LDS exchange is read before the next tile's loads land
   }
 }
