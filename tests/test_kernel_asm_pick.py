@@ -19,3 +19,11 @@ def asm(tmp_path_factory):
 @pytest.mark.parametrize("kernel, picks", [(PICK, True), (REDO, False), (GEMM, False)])
 def test_pick_code_where_it_runs(asm, kernel, picks):
     assert any(op == "ds_write_b128" for _, op, _ in _body(asm, kernel)) == picks
+
+
+@pytest.mark.parametrize("width, waves", [(32, 1), (64, 2)])
+def test_float32_pick_code_where_it_runs(asm, width, waves):
+    name = "_ZN6fastrl15f32_gemm_kernelILi0ELi256ELi%dELi4ELi%dELi2ELb%dEEEvNS_10GemmParamsE"
+    for picks in (False, True):
+        ops = [op for _, op, _ in _body(asm, name % (width, waves, picks))]
+        assert any(op == "ds_write_b128" for op in ops) == picks
