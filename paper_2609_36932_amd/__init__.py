@@ -518,7 +518,9 @@ def _out(out, T, N, dtype, like):
 def matmul_i8(x, x_scale, w, w_scale, *, K=None, out_dtype=None, out=None):
     """Product of int8 codes ``x`` [T, Kp] and ``w`` [N, Kp] (see ``quantize_rows``) with a scale
     per token and output channel: [T, N] in ``out_dtype`` (bfloat16 if not given) or into
-    ``out``, whose rows may be strided.  ``K``: columns that count (all of x's if not given)."""
+    ``out``, whose rows may be strided.  ``K``: columns that count (all of x's if not given); the
+    codes from column K up to the next multiple of 16 are multiplied too, and so have to be 0 in x or in
+    w (``quantize_rows`` writes them so)."""
     stated = K is not None
     K = K if stated else x.shape[1]
     T, ldx = _codes_check(x, x_scale, K, "x", longer=stated)

@@ -47,3 +47,18 @@ def test_widths_that_belong_together(fr):
     q, s = fr.quantize_rows(x)
     assert torch.equal(fr.matmul_i8(q, s, w, ws), ref)
     assert torch.equal(fr.matmul_i8(q, s, wide[:, 32:], ws, K=20), ref)
+
+
+@pytest.mark.parametrize("T", [3, 40, 300])
+def test_codes_past_the_stated_columns(fr, T):
+    """Those up to the next multiple of 16 count unless they are 0 in one operand; later ones never do."""
+    g = torch.Generator().manual_seed(T)
+    x, w = (torch.randint(-128, 128, (n, 64), generator=g, dtype=torch.int32).to(torch.int8) for n in (T, 70))
+    one = torch.ones(300, device=DEV)
+    def product(x, w):
+        return fr.matmul_i8(x.to(DEV), one[:T], w.to(DEV), one[:70], K=20, out_dtype=torch.float32).cpu()
+    exp = lambda n: (x[:, :n].double() @ w[:, :n].double().t()).float()
+    assert torch.equal(product(x, w), exp(32))
+    for a, b in ((x.clone(), w), (x, w.clone())):
+        (a if b is w else b)[:, 20:32] = 0
+        assert torch.equal(product(a, b), exp(20))
