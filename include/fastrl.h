@@ -385,8 +385,8 @@ int fastrl_quantize_rows(const void* x, int32_t dtype, const int32_t* row_index,
  * depend on the rows beside it.
  *   x [T][ldx], w [N][ldw] codes, 16-byte aligned; ldx, ldw multiples of 16, at least K
  *   rounded up to 16, ldw < 2^28; codes from column K up to that multiple of 16 must be 0 in
- *   x or in w (fastrl_quantize_rows writes them so).  T <= 2^31 - 1024, N < 2^30.  out [T][ldo], ldo >= N, in out_dtype, aligned to
- *   its elements; columns from N on are not written.
+ *   x or in w (fastrl_quantize_rows writes them so).  T <= 2^31 - 1024, N < 2^30.  out [T][ldo],
+ *   ldo >= N, in out_dtype, aligned to its elements; columns from N on are not written.
  * fastrl_linear_i8 -- both calls in one: the rows x[row_index[t]] (or x[t]) are coded into the
  *   workspace and multiplied.  x [rows][ldx] in dtype, ldx >= K.  Calls of at most four tokens
  *   and few channels need no workspace (size 0: ws may be NULL).
@@ -410,8 +410,8 @@ int fastrl_linear_i8(const void* x, int32_t dtype, const int32_t* row_index, int
  * with a logit that is NaN or +infinity, or none above -infinity (status FASTRL_SB_BAD_TEACHER,
  * lse NaN), entries are id -1 and logit -infinity, which fastrl_distill_loss_fwd_bwd leaves out.
  *   hidden [rows][d] dense in dtype; W [V][ldw] int8 as for fastrl_matmul_i8; K in [1, 128];
- *   temperature > 0.  No [T, V] array exists: the work runs in slabs of at most 4096 tokens, whose
- *   float32 logits the workspace holds (2.5 GB at V = 152064).
+ *   temperature > 0.  The work runs in slabs of at most 4096 tokens, even shares; the workspace has
+ *   room for one slab's float32 logits (2.5 GB at V = 152064), most of which large calls never write.
  * ------------------------------------------------------------------------------------ */
 size_t fastrl_teacher_topk_workspace_size(int64_t T, int32_t d, int32_t V);
 int fastrl_teacher_topk(const void* hidden, int32_t dtype, const int32_t* row_index,
@@ -443,6 +443,10 @@ int fastrl_teacher_topk(const void* hidden, int32_t dtype, const int32_t* row_in
  *   bfloat16 dW needs bfloat16 operands, is rounded once and cannot be accumulated into
  *   (FASTRL_ERR_UNSUPPORTED); a float32 dW is overwritten, or added to with dW_accumulate.
  *   K in [1, 128]; temperature > 0; loss_scale finite.
+ * Precision: sums are float32 or wider.  With bfloat16 operands both gradients, of either type, carry one
+ *   rounding of dz's entries to bfloat16, and dW one of c_t hidden as well (as in
+ *   fastrl_policy_loss_fwd_bwd).  loss and token_loss are the same with and without gradients asked for, but
+ *   for the order of float32 sums.
  * Slabs of at most slab_tokens tokens (0 = 32768), even shares; workspace as for
  * fastrl_policy_loss_fwd_bwd, and V * d * 4 bytes for a bfloat16 dW of several slabs.
  * ------------------------------------------------------------------------------------ */

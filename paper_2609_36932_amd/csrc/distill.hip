@@ -10,6 +10,12 @@
 //   E_{y_k} <- (p_k - q_k / Q) exp(l - s),
 // formed here in 64 bits from the float32 logit, so that where the student has come close to the
 // teacher the small difference is rounded once, and not two large terms.
+//
+// Roundings to bf16 (bf16 operands, whatever the gradients' type): E, and in dW c h, operands of 16-bit matrix
+// products; then a bf16 result once, from float32 sums.  Against 64 bits, relative: dhidden 0.0024, dW 0.0029 (a
+// float32 computation rounded once: 0.0017).  c h would be exact for a power of two c, which needs l before E is
+// written; E scaled by what is left of c afterwards would be rounded again, in a pass that costs 6%; float16 operands
+// lack the range of exp(z / tau).
 #include <algorithm>
 #include <cmath>
 #include <string>
@@ -240,7 +246,8 @@ __global__ __launch_bounds__(256) void distill_loss_kernel(const DistillParams p
     distill_token(p, int(tl));
 }
 
-// loss = sum of the tokens' terms: a contiguous share per thread, then the threads in order
+// loss = sum of the tokens' terms in a fixed order: every 1024th to a thread, the threads of a wavefront by butterflies,
+// then the wavefronts in order
 __global__ __launch_bounds__(1024) void distill_final_kernel(const double* __restrict__ term, int64_t T,
                                                              float* __restrict__ loss) {
   __shared__ double red[16];

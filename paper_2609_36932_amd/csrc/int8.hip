@@ -403,8 +403,9 @@ __device__ __forceinline__ void i8_tile(const I8Params& p, int mb, int n0, uint1
 // read as 16 codes: 2,640 TOP/s at 16384^3 (bf16 1,564 by the vendor's library, int8 2,265), 2,410 in the product
 // of 8191 tokens at 7B, whose 28 K steps a tile bear a start and an epilogue of ~8 us.  Blocks that walk several
 // tiles and load the next one's first stages during the epilogue measured 5% slower (the stores have to
-// be waited for); two blocks a compute unit, of 128 channels x 192 tokens in two stages of 40 KB each, 18% faster at
-// K = 320 (2433 x 78592 products in bf16: 171 / 150 us), 6% at 640, 6% slower at 1536 and 15% at 3584.
+// be waited for); two blocks a compute unit, of 128 channels x 192 tokens in two stages of 40 KB each, took 12% less
+// time at K = 320 (2433 x 78592 products in bf16: 171 / 150 us), 6% less at 640, 6% more at 1536 and 15% at 3584: not
+// kept, a main loop of its own for K below about 1000 alone.
 // Tiles of 256 output channels x `width` tokens, the last column as narrow as its tokens allow; the last tiles,
 // which do not fill the chip, cut into pieces of fewer tokens (tile_plan).
 template <bool PART>

@@ -1267,7 +1267,8 @@ __global__ __launch_bounds__(THREADS) void loss_kernel(const LossParams p) {
 
 // out[c][r] = scale(r) * in[row(r)][c], zero for r in [R, Rpad): 64 x 64 tiles through LDS with
 // 16-byte global loads and stores (C is a multiple of 8, in 16-byte aligned, Rpad and ldo
-// multiples of 64, out 256-byte aligned)
+// multiples of 64, out 256-byte aligned).  A scaled row is rounded to bf16 again: it is an operand of dW's
+// 16-bit product (distill.hip has what that costs, and why c_t is not in E)
 __global__ __launch_bounds__(256) void transpose_scale_kernel(
     const uint16_t* __restrict__ in, const int32_t* __restrict__ row_index, int64_t row_base,
     int32_t R, int32_t Rpad, int32_t C, const float* __restrict__ scale, uint16_t* __restrict__ out,
