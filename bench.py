@@ -60,7 +60,8 @@ def parse():
 
 
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "lmhead_qwen2.5-vl-7b_grpo_hbm_traffic.md")
-KERNEL_SRCS = [os.path.join(ROOT, "paper_2609_36932_amd", "csrc", f) for f in ("lmhead.hip", "gemm_loop.h")]
+KERNEL_SRCS = [os.path.join(ROOT, "paper_2609_36932_amd", "csrc", f)
+               for f in ("lmhead.hip", "lmhead.h", "gemm_loop.h", "common.h")]
 
 
 def kernel_source_hash():
