@@ -1,5 +1,6 @@
 """bench.py reports recorded memory traffic only while the sources that the counters were taken of are the same:
-every file that the measured kernels are compiled from has to be among those it looks at."""
+every file of the kernels' folder that they are compiled from has to be among those it looks at (the public header
+declares entry points and numbers of the interface)."""
 import os
 import re
 
@@ -9,7 +10,7 @@ CSRC = os.path.join(bench.ROOT, "paper_2609_36932_amd", "csrc")
 
 
 def _included(name, seen):
-    if name not in seen and os.path.exists(os.path.join(CSRC, name)):
+    if name not in seen and name in os.listdir(CSRC):
         seen.add(name)
         for inc in re.findall(r'^#include "([^"]+)"', open(os.path.join(CSRC, name)).read(), re.M):
             _included(inc, seen)
