@@ -402,8 +402,8 @@ __device__ __forceinline__ void i8_tile(const I8Params& p, int mb, int n0, uint1
 // The matrix product of many tokens, on the main loop of the bf16 GEMMs (gemm_loop.h) with its 16-byte pieces
 // read as 16 codes: 2,640 TOP/s at 16384^3 (bf16 1,564 by the vendor's library, int8 2,265), 2,410 in the product
 // of 8191 tokens at 7B, whose 28 K steps a tile bear a start and an epilogue of ~8 us.  Blocks that walk several
-// tiles and load the next one's first stages during the epilogue measured 5% slower (the stores have to
-// be waited for); two blocks a compute unit, of 128 channels x 192 tokens in two stages of 40 KB each, took 12% less
+// tiles and load the next one's first stages during the epilogue measured 5% slower (in a form that waited for
+// the stores, and spilled); two blocks a compute unit, of 128 channels x 192 tokens in two stages of 40 KB each, took 12% less
 // time at K = 320 (2433 x 78592 products in bf16: 171 / 150 us), 6% less at 640, 6% more at 1536 and 15% at 3584: not
 // kept, a main loop of its own for K below about 1000 alone.
 // Tiles of 256 output channels x `width` tokens, the last column as narrow as its tokens allow; the last tiles,
@@ -821,10 +821,10 @@ static int check_product(const char* fn, const void* x, int64_t ldx, const void*
 }
 
 // Calls of few tokens and channels code the rows in the kernel that multiplies them and leave the workspace alone.
-// linear_i8 in bf16, us, two launches / one (mostly the caller's time): 1 x 1536 x 1536 (T x N x K) 12.8 / 9.0, 16 x
-// 1536 x 1536 12.8 / 9.8, 16 x 3584 x 3584 13.0 / 11.7, 8 x 3584 x 6000 13.3 / 11.6.  Not where one wavefront would have
-// more than 7168 columns to code (12 x 300 x 5000 13.0 / 13.6, 5 x 300 x 8192 13.5 / 14.6), or the blocks
-// together more than 230M (8 x 8000 x 4500 13.0 / 15.4, 16 x 32000 x 1536 14.0 / 28.8).
+// linear_i8 in bf16, us, two launches / one (mostly the caller's time): 1 x 1536 x 1536 (T x N x K) 12.2 / 8.9, 16 x
+// 1536 x 1536 12.3 / 10.2, 16 x 3584 x 3584 12.2 / 11.2, 8 x 3584 x 6000 12.2 / 11.8.  Not where one wavefront would have
+// more than 7168 columns to code (11 x 300 x 5000 12.4 / 13.3, 5 x 300 x 8192 12.3 / 14.5), or the blocks
+// together more than 230M (8 x 8000 x 4500 12.1 / 14.7, 16 x 32000 x 1536 13.6 / 28.5).
 static bool one_launch(int64_t T, int32_t N, int32_t K) {
   if (T > 16 || N >= 8192 || K > 32768) return false;
   const int64_t Kp = rup(K, 16);
